@@ -4,12 +4,15 @@
 // head after head, so that those sums stay in registers from plane to plane of a head.  Per plane, all threads together:
 //   norm     thread = row: K and Q scaled to unit rows in place, each value as two bf16, it and what rounding it left off (`rest`), so
 //            that the states are as good as those of fp32 rows: the gradients are made of them alone
+//            (K and Q come once more, from L2, when the states have been taken: a unit row rounded to one bf16, in a dot product whose result is
+//            taken off the row, leaves 2^-9 of what should have cancelled: rows of cosine 0.97 with a common direction, dq off by 7.8e-3
+//            instead of 1.7e-3)
 //   state    UMMAs: [K^ Q^]^T [V G], whose diagonal blocks are S and T (one contraction of 2 W x 2 W reads each operand once; two of W x W with a row
 //            of ones took 1.5 times as long), values and rests one after the other, and a row of ones times G: the token sum
 //   operand  S' = S / pi and T' = T / pi from TMEM, as pairs of bf16 again, over the rests, which are dead
-//   products UMMAs, over the states' columns: G S'^T, K^ T' and V T'^T, 128 rows each
-//   rows     thread = row: dq = (g^ - q^ (q^ . g^)) / |q| from the accumulator and the row of Q^, over it in place, stored by TMA; dk likewise
-//   values   K^ T' rows to shared memory as fp32 (over the rests), then lane = channel pair, warp = strip of two columns (width 32: four):
+//   products UMMAs, over the states' columns: G S'^T, V T'^T and K T', 128 rows each
+//   rows     thread = row: dq = (g^ - q^ (q^ . g^)) / |q| from the accumulator and the row of Q, over it in place, stored by TMA; dk likewise
+//   values   K T' rows over |k| to shared memory as fp32 (over the rests), then lane = channel pair, warp = strip of two columns (width 32: four):
 //            the convolution of G with the filters turned around slides down the strip; the same window of G times the value at its
 //            centre gives the filters' sums
 // ROOMY: the token grid with its halo fits a buffer: for the values G and V come once more (from L2), over the first copies, without swizzle and with
@@ -72,11 +75,11 @@ tc_grad_fused_kernel(const __grid_constant__ Maps maps, const FusedParams prm) {
     float* len_s = reinterpret_cast<float*>(smem + G::kOffLen);      // [2][kTokens]: of K, of Q; negative: a row not longer than eps
     float* sum_s = reinterpret_cast<float*>(smem + G::kOffSum);
     float* w_s = reinterpret_cast<float*>(smem + G::kOffW);
-    uint64_t* kq_full = reinterpret_cast<uint64_t*>(smem + G::kOffBar);
+    uint64_t* kq_full = reinterpret_cast<uint64_t*>(smem + G::kOffBar);     // twice a plane
     uint64_t* vg_full = kq_full + 1;
     uint64_t* state_done = kq_full + 2;
     uint64_t* q_done = kq_full + 3;      // G S'^T
-    uint64_t* all_done = kq_full + 4;    // K^ T' and V T'^T too
+    uint64_t* all_done = kq_full + 4;    // V T'^T and K T' too
     uint64_t* grid_full = kq_full + 5;   // V and G without swizzle
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(kq_full + 6);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -141,7 +144,7 @@ tc_grad_fused_kernel(const __grid_constant__ Maps maps, const FusedParams prm) {
         const uint32_t ph = it & 1;
         const int plane = first + it, h = plane / prm.B, b = plane - h * prm.B;
         // ---- norm ----
-        ok = mbar_wait(kq_full, ph, abort_flag, prm.status, kBit);
+        ok = mbar_wait(kq_full, 0, abort_flag, prm.status, kBit);
         if (!__syncthreads_and(ok)) break;
         if (it == 0 || b == 0)      // the head's first plane here
             for (int i = tid; i < kTaps * W; i += kThreads) w_s[(kTaps - 1 - i % kTaps) * W + i / kTaps] = __bfloat162float(prm.w[(size_t)h * W * kTaps + i]);
@@ -198,6 +201,8 @@ tc_grad_fused_kernel(const __grid_constant__ Maps maps, const FusedParams prm) {
         }
         ok = mbar_wait(state_done, ph, abort_flag, prm.status, kBit);
         if (!__syncthreads_and(ok)) break;
+        if (tid == 0) { load_kq(it); ++issued_kq; }     // over the unit rows, which are dead
+        __syncwarp();
         tcgen05_fence_after_sync();
 
         // ---- operands: rows of S in the lower lanes, of T in the upper ones; a warp takes 16 columns of its lanes at a time ----
@@ -234,7 +239,7 @@ tc_grad_fused_kernel(const __grid_constant__ Maps maps, const FusedParams prm) {
         tcgen05_fence_before_sync();
         __syncthreads();
 
-        // ---- products: columns [0, tiles) W of G S'^T, then K^ T', then V T'^T ----
+        // ---- products: columns [0, tiles) W of G S'^T, then K T', then V T'^T ----
         if (warp == kWarps - 1) {     // one of a team whose rows have to wait for all of them
             tcgen05_fence_after_sync();
             if (elect_one()) {
@@ -254,14 +259,17 @@ tc_grad_fused_kernel(const __grid_constant__ Maps maps, const FusedParams prm) {
                 };
                 product(0, at_g, S, true);
                 umma_commit(q_done);
-                product(1, at_k, T, false);
                 product(2, at_v, T, true);
-                umma_commit(all_done);
+                if (mbar_wait(kq_full, 1, abort_flag, prm.status, kBit)) {
+                    product(1, at_k, T, false);
+                    umma_commit(all_done);
+                }
             }
             __syncwarp();
         }
 
         // ---- rows: a team of four warps takes a tile of dq, or of dk ----
+        ok = mbar_wait(kq_full, 1, abort_flag, prm.status, kBit);
         for (int task = team; task < 2 * tiles; task += kWarps / 4) {
             const int side = task < tiles ? 1 : 0, t = task < tiles ? task : task - tiles, r = t * kTile + quarter * 32 + lane;   // dq first
             ok = ok && mbar_wait(side ? q_done : all_done, ph, abort_flag, prm.status, kBit);
@@ -295,7 +303,7 @@ tc_grad_fused_kernel(const __grid_constant__ Maps maps, const FusedParams prm) {
                         for (int i = 0; i < 4; ++i) dot2 = fma2(unpack2(w4[i]), v[i], dot2);
                     });
                 const float rn = len_s[side * G::kTokens + r];
-                const f2 along2 = pair(rn > 0.f ? -both(dot2) : 0.f), rn2 = pair(fabsf(rn));
+                const f2 along2 = pair(rn > 0.f ? -both(dot2) * rn * rn : 0.f), rn2 = pair(fabsf(rn));
 #pragma unroll
                 for (int col = 0; col < W; col += 32)
                     columns(col, [&](int j, const uint32_t (&w4)[4], const f2 (&v)[4]) {
@@ -314,7 +322,7 @@ tc_grad_fused_kernel(const __grid_constant__ Maps maps, const FusedParams prm) {
                 }
             }
         }
-        // ---- values: K^ T' rows over the rests, as fp32 (swizzled: 16-byte chunk c of row r at chunk c ^ (r & 7)), by the teams of dq ----
+        // ---- values: K T' rows over |k|, over the rests, as fp32 (swizzled: 16-byte chunk c of row r at chunk c ^ (r & 7)), by the teams of dq ----
         ok = ok && mbar_wait(all_done, ph, abort_flag, prm.status, kBit);
         ok = __all_sync(0xffffffffu, ok);
         if (ok) {
@@ -333,9 +341,10 @@ tc_grad_fused_kernel(const __grid_constant__ Maps maps, const FusedParams prm) {
                 tmem_ld_wait();
                 if (ROOMY && r >= N) continue;      // padded rows of all tiles would not fit
                 uint8_t* row = smem + G::kOffRest + r * G::kLine;
+                const float rk = fabsf(len_s[r]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    *reinterpret_cast<float4*>(row + (((c0 * 4 + e) ^ (ROOMY ? 0 : r & 7)) << 4)) = make_float4(a[4 * e], a[4 * e + 1], a[4 * e + 2], a[4 * e + 3]);
+                    *reinterpret_cast<float4*>(row + (((c0 * 4 + e) ^ (ROOMY ? 0 : r & 7)) << 4)) = make_float4(a[4 * e] * rk, a[4 * e + 1] * rk, a[4 * e + 2] * rk, a[4 * e + 3] * rk);
             }
             tcgen05_fence_before_sync();
         }
