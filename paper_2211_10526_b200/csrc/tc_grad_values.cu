@@ -5,10 +5,12 @@
 // the convolution slides down a patch is the one that V at its centre is multiplied with for the filters, so G is read once for both.
 // Persistent CTAs walk a contiguous range of 8 x 16-token patches.  Per patch
 //   warp 0       TMA: the patch of K (swizzled), that of G with its halo and that of V with the same halo; noughts outside the grid
-//   warp 1       UMMAs: acc[128 x 64] = K[128 x 64] T'[64 x 64] into TMEM, T' = T / pi in bf16
+//   warp 1       UMMAs: acc[128 x 64] = K[128 x 64] T'[64 x 64] into TMEM, T' = T / pi as two bf16, it and what rounding it left off (one bf16
+//                alone is as large an error as the result's own rounding where G's token sum is small)
 //   warps 2..5   thread = token: 1 / |k|, the accumulator row from TMEM, dv = acc / max(|k|, eps) + staged, stored with TMA
 //   warps 6..13  lane = channel pair, a pair of columns each: the convolution of G (+ half of its token sum), staged in shared memory as fp32,
-//                and the filters' sums, in registers from patch to patch of a plane; at its end the warps' sums are added up and written
+//                and the filters' sums, in registers from patch to patch of a plane; at its end the warps' sums are added up, in a staging buffer
+//                that is free, and written
 // One kernel for both took the place of the apply kernel and one for the filters alone: 2 x 8 planes of 256 x 256, 78 us and 207 us.
 #include "grad.cuh"
 #include "tc_common.cuh"
@@ -26,9 +28,11 @@ constexpr int kStgStride = kD * 4 + 16, kStgBytes = kTile * kStgStride;      // 
 constexpr int kEpiThreads = 128, kConvWarps = 8, kConvThreads = kConvWarps * 32, kThreads = 64 + kEpiThreads + kConvThreads;
 constexpr int kTmemCols = 128;                                               // two accumulators
 constexpr int kSumWords = (kTaps + 1) * kD;
-// T' | dv patch | stages | staging x2 | warps' sums of the filters, four at a time | barriers
-constexpr int kOffT = 0, kOffOut = 8192, kOffStages = kOffOut + kKBytes, kOffStg = kOffStages + kStages * kStage;
-constexpr int kOffSums = kOffStg + 2 * kStgBytes, kOffBar = kOffSums + kConvWarps / 2 * kSumWords * 4;
+// T' (two halves) | dv patch | stages | staging x2 | barriers
+constexpr int kOperand = kD * kRow;
+constexpr int kOffT = 0, kOffOut = 2 * kOperand, kOffStages = kOffOut + kKBytes, kOffStg = kOffStages + kStages * kStage;
+constexpr int kOffBar = kOffStg + 2 * kStgBytes;
+static_assert(kConvWarps * kSumWords * 4 <= kStgBytes, "the warps' sums of the filters in a staging buffer");
 constexpr size_t kSmem = 1024 + kOffBar + 256;
 static_assert(kSmem <= 227 * 1024, "shared memory");
 
@@ -68,7 +72,6 @@ tc_grad_values_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     uint8_t* out_s = smem + kOffOut;
     uint8_t* stages = smem + kOffStages;
     uint8_t* stg = smem + kOffStg;
-    float* sums_s = reinterpret_cast<float*>(smem + kOffSums);
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + kOffBar);    // [NS] TMA landed
     uint64_t* empty = full + NS;                                     // [NS] stage consumed (convolution and epilogue threads, UMMA commit)
     uint64_t* acc_full = empty + NS;                                 // [2]  UMMAs retired
@@ -118,7 +121,7 @@ tc_grad_values_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         }
     } else if (warp == 1) {
         constexpr uint32_t idesc = umma_idesc_bf16(128, kD, false, true);
-        const uint32_t t_low = desc_low(smem_u32(T_s));
+        const uint32_t t_low = desc_low(smem_u32(T_s)), t_rest = desc_low(smem_u32(T_s) + kOperand);
         int prev = -1, seg = 0;
         PatchWalk pw(g_begin, prm.tilesX, prm.tilesY);
         for (int it = 0; it < my_tiles; ++it, pw.step(prm.tilesX, prm.tilesY)) {
@@ -133,7 +136,9 @@ tc_grad_values_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             if (elect_one()) {
                 const uint32_t k_low = desc_low(smem_u32(stages + s * kStage));
 #pragma unroll
-                for (int k = 0; k < kD / 16; ++k) umma_bf16_low(tmem + b * kD, k_low + k * 2, t_low + k * (2048u >> 4), idesc, k != 0);
+                for (int k = 0; k < kD / 16; ++k) umma_bf16_low(tmem + b * kD, k_low + k * 2, t_rest + k * (2048u >> 4), idesc, k != 0);
+#pragma unroll
+                for (int k = 0; k < kD / 16; ++k) umma_bf16_low(tmem + b * kD, k_low + k * 2, t_low + k * (2048u >> 4), idesc, 1u);
                 umma_commit(&acc_full[b]);
                 umma_commit(&empty[s]);
             }
@@ -156,10 +161,14 @@ tc_grad_values_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const float4 lo = __ldg(src + 2 * c), hi = __ldg(src + 2 * c + 1);
-                    uint4 o;
+                    uint4 o, r;
                     o.x = pack_bf16x2(lo.x * kInvPi, lo.y * kInvPi); o.y = pack_bf16x2(lo.z * kInvPi, lo.w * kInvPi);
                     o.z = pack_bf16x2(hi.x * kInvPi, hi.y * kInvPi); o.w = pack_bf16x2(hi.z * kInvPi, hi.w * kInvPi);
-                    *reinterpret_cast<uint4*>(T_s + i * kRow + (((part * 4 + c) ^ (i & 7)) << 4)) = o;
+                    r.x = rest_bf16x2(lo.x, lo.y, kInvPi, o.x); r.y = rest_bf16x2(lo.z, lo.w, kInvPi, o.y);
+                    r.z = rest_bf16x2(hi.x, hi.y, kInvPi, o.z); r.w = rest_bf16x2(hi.z, hi.w, kInvPi, o.w);
+                    uint8_t* to = T_s + i * kRow + (((part * 4 + c) ^ (i & 7)) << 4);
+                    *reinterpret_cast<uint4*>(to) = o;
+                    *reinterpret_cast<uint4*>(to + kOperand) = r;
                 }
                 fence_proxy_async_smem();
                 mbar_arrive(t_ready);
@@ -222,40 +231,30 @@ tc_grad_values_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         f2 w[kTaps], dw[kTaps], db = 0ull, half = 0ull;    // filters turned around, and the sums that go with them
 #pragma unroll
         for (int i = 0; i < kTaps; ++i) w[i] = dw[i] = 0ull;
-        // the warps' sums of a plane to its slot, four warps' at a time
-        auto flush = [&](int plane) {
+        // the warps' sums of a plane to its slot, through staging buffer b, which the epilogue has left
+        auto flush = [&](int plane, int b) {
+            float* sums_s = reinterpret_cast<float*>(stg + b * kStgBytes);
             float* to = prm.sums + (size_t)(plane + (int)blockIdx.x) * kSumWords;
-            float mine[(kSumWords + kConvThreads - 1) / kConvThreads];
+            f2* at = reinterpret_cast<f2*>(sums_s + cw * kSumWords) + lane;
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                if (cw / 4 == part) {
-                    f2* at = reinterpret_cast<f2*>(sums_s + (cw & 3) * kSumWords) + lane;
-#pragma unroll
-                    for (int i = 0; i < kTaps; ++i) at[i * 32] = dw[kTaps - 1 - i];
-                    at[kTaps * 32] = db;
-                }
-                named_barrier_sync(2, kConvThreads);
-#pragma unroll
-                for (int j = 0; j < (kSumWords + kConvThreads - 1) / kConvThreads; ++j) {
-                    const int i = ct + j * kConvThreads;
-                    if (part == 0) mine[j] = 0.f;
-                    if (i < kSumWords)
-                        for (int k = 0; k < 4; ++k) mine[j] += sums_s[k * kSumWords + i];
-                    if (part == 1 && i < kSumWords) to[i] = mine[j];
-                }
-                named_barrier_sync(2, kConvThreads);
-            }
-#pragma unroll
-            for (int i = 0; i < kTaps; ++i) dw[i] = 0ull;
+            for (int i = 0; i < kTaps; ++i) { at[i * 32] = dw[kTaps - 1 - i]; dw[kTaps - 1 - i] = 0ull; }
+            at[kTaps * 32] = db;
             db = 0ull;
+            named_barrier_sync(2, kConvThreads);
+            for (int i = ct; i < kSumWords; i += kConvThreads) {
+                float s = 0.f;
+                for (int k = 0; k < kConvWarps; ++k) s += sums_s[k * kSumWords + i];
+                to[i] = s;
+            }
+            named_barrier_sync(2, kConvThreads);
         };
         int prev = -1;
         bool ok = true;
         PatchWalk pw(g_begin, prm.tilesX, prm.tilesY);
         for (int it = 0; it < my_tiles; ++it, pw.step(prm.tilesX, prm.tilesY)) {
             const int s = it % NS, use = it / NS, b = it & 1, ub = it >> 1;
+            const int done = prev;
             if (pw.bh != prev) {
-                if (prev >= 0 && prm.dw) flush(prev);
                 prev = pw.bh;
                 const int ch = pw.bh % prm.H * kD + 2 * lane;
 #pragma unroll
@@ -267,6 +266,7 @@ tc_grad_values_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             ok = mbar_wait(&full[s], use & 1, abort_flag, prm.status, kBit);
             ok = ok && (ub == 0 || mbar_wait(&buf_free[b], (ub - 1) & 1, abort_flag, prm.status, kBit));
             if (named_barrier_any(2, kConvThreads, !ok)) break;     // together: the sums' barriers take all of them
+            if (prm.dw && done >= 0 && done != prev) flush(done, b);
             const uint32_t g_at = smem_u32(stages + s * kStage + kKBytes) + 2 * cw * kRow + lane * 4, v_at = g_at + kHaloBytes + (HX + R) * kRow;
             const uint32_t to = smem_u32(stg + b * kStgBytes) + 2 * cw * kStgStride + lane * 8;
             constexpr int NIN = KS + 1;
@@ -318,7 +318,11 @@ tc_grad_values_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             mbar_arrive(&empty[s]);
             mbar_arrive(&conv_full[b]);
         }
-        if (ok && prev >= 0 && prm.dw) flush(prev);
+        if (prm.dw && prev >= 0) {
+            const int b = my_tiles & 1, ub = my_tiles >> 1;
+            ok = ok && (ub == 0 || mbar_wait(&buf_free[b], (ub - 1) & 1, abort_flag, prm.status, kBit));
+            if (!named_barrier_any(2, kConvThreads, !ok)) flush(prev, b);
+        }
     }
     tcgen05_fence_before_sync();
     __syncthreads();
