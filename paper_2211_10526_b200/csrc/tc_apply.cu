@@ -55,6 +55,7 @@ template <int KS> struct Geo {
     // staging buffer
     static constexpr int kOffS2 = ((kOffBar + 256 + 1023) / 1024) * 1024, kOffHs = kOffS2 + 8192;
     static constexpr size_t kSmemRN = 1024 + kOffHs + 2 * kD * 4;
+    static constexpr size_t kSmemFine = 1024 + kOffHs;       // what rounding the operand left off, in the place of that second block
 };
 
 struct ApplyParams {
@@ -88,7 +89,9 @@ struct PatchWalk {
 // RN: row-sum normalisation (Eq. 3's denominator on the kept kernel of Eq. 8).  The state carries sum_n k^_n behind s; the
 // operand gets one more column (sum k^ / pi), so that column 64 of the accumulator is q . sum k^ / pi; the attention term (acc / ||q|| + 1/2 s) is divided by n_tokens / 2 + that product
 // / ||q|| before the convolution and the bias are added.
-template <int KS, bool RN>
+// FINE (gradients): the operand as two bf16, it and what rounding it left off, contracted one after the other: one bf16 alone is as large an
+// error as the result's own rounding where the token sum and the convolution are small.
+template <int KS, bool RN, bool FINE>
 __global__ void __launch_bounds__(Geo<KS>::kThreads, 1)
 tc_apply_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmV,
                 const __grid_constant__ CUtensorMap tmO, const ApplyParams prm) {
@@ -104,7 +107,7 @@ tc_apply_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     uint8_t* stages = smem + G::kOffStages;
     uint8_t* stg = smem + G::kOffStg;
     float* rq_s = reinterpret_cast<float*>(smem + G::kOffRq);
-    uint8_t* S2_s = smem + G::kOffS2;                                  // RN only
+    uint8_t* S2_s = smem + G::kOffS2;                                  // RN: the second block; FINE: the rest
     float* hs_s = reinterpret_cast<float*>(smem + G::kOffHs);          // RN only: [2][64]
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + G::kOffBar);  // [NS] TMA landed
     uint64_t* empty = full + NS;                                      // [NS] stage consumed (conv + epilogue warps, UMMA commit)
@@ -170,6 +173,7 @@ tc_apply_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         constexpr uint32_t idesc = umma_idesc_bf16(128, kAccN, false, true);
         const uint32_t s_addr = smem_u32(S_s);
         const uint32_t s_low = desc_low(s_addr, RN ? smem_u32(S2_s) - s_addr : 0);   // lbo: to the operand's second 64-wide block
+        const uint32_t rest_low = FINE ? desc_low(smem_u32(S2_s)) : 0;
         int prev_bh = -1, seg = 0;
         PatchWalk pw(g_begin, prm.tilesX, prm.tilesY);
         for (int it = 0; it < my_tiles; ++it, pw.step(prm.tilesX, prm.tilesY)) {
@@ -184,9 +188,13 @@ tc_apply_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             tcgen05_fence_after_sync();
             if (elect_one()) {
                 const uint32_t q_low = desc_low(smem_u32(stages + s * G::kStage));   // K-major rows of 128 B
+                if (FINE) {
+#pragma unroll
+                    for (int k = 0; k < kD / 16; ++k) umma_bf16_low(tmem + b * kAcc, q_low + k * 2, rest_low + k * (2048u >> 4), idesc, k != 0);
+                }
 #pragma unroll
                 for (int k = 0; k < kD / 16; ++k)   // the operand is N-major, 16 K-rows per step
-                    umma_bf16_low(tmem + b * kAcc, q_low + k * 2, s_low + k * (2048u >> 4), idesc, k != 0);
+                    umma_bf16_low(tmem + b * kAcc, q_low + k * 2, s_low + k * (2048u >> 4), idesc, FINE || k != 0);
                 umma_commit(&acc_full[b]);
                 umma_commit(&empty[s]);  // the same UMMAs have finished reading the Q patch
             }
@@ -217,6 +225,12 @@ tc_apply_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                     o.x = pack_bf16x2(lo.x * kInvPi, lo.y * kInvPi); o.y = pack_bf16x2(lo.z * kInvPi, lo.w * kInvPi);
                     o.z = pack_bf16x2(hi.x * kInvPi, hi.y * kInvPi); o.w = pack_bf16x2(hi.z * kInvPi, hi.w * kInvPi);
                     *reinterpret_cast<uint4*>(S_s + i * 128 + (((part * 2 + c) ^ (i & 7)) << 4)) = o;
+                    if (FINE) {
+                        uint4 r;
+                        r.x = rest_bf16x2(lo.x, lo.y, kInvPi, o.x); r.y = rest_bf16x2(lo.z, lo.w, kInvPi, o.y);
+                        r.z = rest_bf16x2(hi.x, hi.y, kInvPi, o.z); r.w = rest_bf16x2(hi.z, hi.w, kInvPi, o.w);
+                        *reinterpret_cast<uint4*>(S2_s + i * 128 + (((part * 2 + c) ^ (i & 7)) << 4)) = r;
+                    }
                     if (RN) {
                         // second block of the operand: row i (a key feature) holds sum k^[i] / pi in column 0; the rest is zero
                         uint4 z = make_uint4(0, 0, 0, 0);
@@ -391,7 +405,7 @@ tc_apply_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     if (warp == 1) tmem_dealloc(tmem, RN ? 2 * kTmemCols : kTmemCols);
 }
 
-template <int KS, bool RN>
+template <int KS, bool RN, bool FINE = false>
 cudaError_t launch_apply_ks(const Problem& p, const float* state, unsigned* status, cudaStream_t st) {
     using G = Geo<KS>;
     CUtensorMap tmQ, tmV, tmO;
@@ -429,10 +443,11 @@ cudaError_t launch_apply_ks(const Problem& p, const float* state, unsigned* stat
     prm.tilesX = (p.gridW + kTX - 1) / kTX; prm.tilesY = (p.gridH + kTY - 1) / kTY;
     prm.n_tiles = p.BH * prm.tilesX * prm.tilesY;
     prm.eps2 = p.eps2; prm.status = status; prm.n_tokens = p.N; prm.v_row0 = p.v_rows > 0 ? p.v_row0 : 0;
-    constexpr size_t kSmemBytes = RN ? G::kSmemRN : G::kSmem;
+    constexpr size_t kSmemBytes = RN ? G::kSmemRN : FINE ? G::kSmemFine : G::kSmem;
+    static_assert(!(RN && FINE) && kSmemBytes <= 227 * 1024, "shared memory");
     static PerDevice opt_in;  // one per instantiation
     {
-        const cudaError_t e = opt_in_smem(tc_apply_kernel<KS, RN>, kSmemBytes, opt_in);
+        const cudaError_t e = opt_in_smem(tc_apply_kernel<KS, RN, FINE>, kSmemBytes, opt_in);
         if (e != cudaSuccess) return e;
     }
     const int sms = device_sm_count();  // one persistent CTA per multiprocessor
@@ -446,7 +461,7 @@ cudaError_t launch_apply_ks(const Problem& p, const float* state, unsigned* stat
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = p.phase != kPhaseApplyOnly;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, tc_apply_kernel<KS, RN>, tmQ, tmV, tmO, prm);
+    return cudaLaunchKernelEx(&cfg, tc_apply_kernel<KS, RN, FINE>, tmQ, tmV, tmO, prm);
 }
 
 // Output rows of the off-grid leading tokens: out = q^ S / pi + 1/2 s (no convolution, no bias), from the
@@ -516,6 +531,7 @@ cudaError_t launch_prefix_rows(const Problem& p, const float* state, cudaStream_
 
 cudaError_t launch_apply(const Problem& p, const float* state, unsigned* status, cudaStream_t st) {
     if (p.d == 32) return launch_apply32(p, state, status, st);
+    if (p.fine) return p.ksize == 5 && !p.rownorm ? launch_apply_ks<5, false, true>(p, state, status, st) : cudaErrorInvalidValue;   // 3x3: tc_grad_values.cu
     if (p.ksize == 3) return p.rownorm ? launch_apply_ks<3, true>(p, state, status, st) : launch_apply_ks<3, false>(p, state, status, st);
     return p.rownorm ? launch_apply_ks<5, true>(p, state, status, st) : launch_apply_ks<5, false>(p, state, status, st);
 }

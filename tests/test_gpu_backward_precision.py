@@ -12,8 +12,9 @@ pytestmark = pytest.mark.gpu
 # one kernel for all gradients: planes of one tile and of two, with a token grid that fits a buffer with its halo and without
 SHORT = [((2, 3, 14, 14, 64, 3), 1), ((2, 3, 14, 14, 64, 3), 0), ((3, 2, 9, 12, 64, 3), 2), ((2, 2, 1, 200, 64, 3), 0), ((2, 2, 16, 16, 64, 3), 0), ((2, 4, 14, 14, 32, 3), 1),
          ((2, 2, 20, 24, 32, 3), 0), ((160, 2, 7, 7, 64, 3), 0), ((2, 2, 1, 100, 64, 3), 3), ((1, 2, 1, 500, 32, 3), 0)]
-# a kernel for the values and one for the rows
-LONG = [((2, 3, 20, 20, 64, 3), 0), ((2, 3, 17, 37, 64, 3), 1), ((1, 2, 80, 70, 64, 3), 0), ((60, 3, 17, 16, 64, 3), 0), ((2, 2, 1, 400, 64, 3), 2), ((1, 3, 30, 33, 32, 3), 1)]
+# a kernel for the values and one for the rows; other filters
+LONG = [((2, 3, 20, 20, 64, 3), 0), ((2, 3, 17, 37, 64, 3), 1), ((1, 2, 80, 70, 64, 3), 0), ((60, 3, 17, 16, 64, 3), 0), ((2, 2, 1, 400, 64, 3), 2), ((1, 3, 30, 33, 32, 3), 1),
+        ((2, 3, 14, 14, 64, 5), 1), ((2, 3, 30, 33, 64, 5), 0), ((40, 4, 17, 17, 64, 5), 2), ((2, 3, 30, 33, 32, 5), 1), ((2, 3, 12, 15, 64, 7), 1), ((2, 3, 12, 15, 64, 1), 0)]
 
 
 def tensors(shape, prefix, cosine, centred, seed):
