@@ -351,7 +351,8 @@ typedef struct {
  *               runs, nothing in it has to be set and nothing is kept.  Calls that run at the same time (other streams,
  *               captured graphs) need one each.
  *   everything else as for castling_attn_forward.  No output may overlap an input or the workspace, nor share elements with
- *   another output (slices of one fused tensor are checked for it); the strides of an output nest: each is at least what the shorter ones reach.
+ *   another output; outputs may lie between one another as slices of one fused tensor do, with the same strides, others may not reach into one
+ *   another.  The strides of an output nest: each is at least what the shorter ones reach.
  *
  * Sums over tokens, images and heads' filters are taken in fp32 in an order that depends on the shape alone: the same call
  * gives the same bits.  All tensors have one dtype, the filters' gradients too (rounded once from fp32 sums).  bf16 heads of width 64
@@ -392,8 +393,9 @@ typedef struct {
 
 /*
  *   q, k, q_out, k_out   DEVICE.  Each output is its input itself (the same address and strides: turned in place) or overlaps neither
- *                        input; the outputs share no elements (slices of one fused tensor are checked for it), and their strides nest:
- *                        each is at least what the shorter ones reach.  Any alignment of elements; strides >= 0, token strides
+ *                        input; the outputs share no elements (they may lie between one another as slices of one fused tensor do, with
+ *                        the same strides; others may not reach into one another), and their strides nest: each is at least what the shorter
+ *                        ones reach.  Any alignment of elements; strides >= 0, token strides
  *                        >= d where N > 1, those of batches and heads > 0 where there are several.  16-byte aligned rows are fastest.
  *   positions            DEVICE, or NULL for CASTLING_POSITIONS_GRID.  Angles are taken in 64 bits: far positions lose nothing.
  * Enqueues one kernel on `stream` of the current device; no workspace, no handle.  Errors: INVALID_ARG, UNSUPPORTED (sizes, dtype),
