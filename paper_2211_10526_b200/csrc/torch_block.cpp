@@ -234,6 +234,8 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int rc = without_gil(*q, [&](void* stream) { return g_rotate(&cfg, qp, kp, qop, kop, pp, stream); });
     if (rc != CASTLING_OK) return PyLong_FromLong(rc);
     if (in_place) {
+        written(*q);
+        if (k) written(*k);
         Py_INCREF(a[4]); Py_INCREF(a[5]);
         return pack<2>({a[4], a[5]});
     }
@@ -345,6 +347,7 @@ PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     PyObject* items[3];
     for (int i = 0; i < 3; ++i) {
         if (a[11] == Py_None) { items[i] = wrap(std::move(made[i])); continue; }
+        written(*out[i]);
         items[i] = PyTuple_GET_ITEM(a[11], i);
         Py_INCREF(items[i]);
     }

@@ -87,7 +87,7 @@ PyObject* forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     PyEval_RestoreThread(gil);
     if (rc != CASTLING_OK) return PyLong_FromLong(rc);
-    if (a[10] != Py_None) { Py_INCREF(a[10]); return a[10]; }
+    if (a[10] != Py_None) { torch_call::written(*out); Py_INCREF(a[10]); return a[10]; }
     return THPVariable_Wrap(std::move(made));
     END_HANDLE_TH_ERRORS
 }

@@ -20,6 +20,11 @@ inline const at::Tensor* tensor(PyObject* o, const char* name) {
     return nullptr;
 }
 
+// A caller's tensor has been written: autograd has to know that what it may have kept of it is gone.
+inline void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 inline PyObject* value_error(const char* what) { PyErr_SetString(PyExc_ValueError, what); return nullptr; }
 
 // torch_block.cpp: the operators around the attention core
