@@ -267,11 +267,15 @@ grad_filter_kernel(const T* __restrict__ g, const T* __restrict__ v, float* __re
 }
 
 // grid (heads * (taps + 1)): adds the slots up, in the order of images and slots, in kParts strands.
+// The kernels before it multiply what lies outside the grid, and rows that have not started yet or have ended, as noughts: an infinity or a NaN on the
+// other side makes a NaN of a product that the definition does not have.  A sum that is a NaN is therefore taken again, term by term as the definition
+// has it, until it is one.  Sums without cost a comparison: 64 x 4 planes of 196 tokens, width 32, 19.8 -> 20.0 us a backward.
 constexpr int kParts = 8;
+struct FilterTerms { const void *g, *v; Layout lg, lv; int hdiv, prefix, gridH, gridW, ksize; };
 template <typename T>
 __global__ void __launch_bounds__(128 * kParts)   // channels, up to a multiple of 32, times strands
 grad_filter_sum_kernel(const float* __restrict__ sums, T* __restrict__ dw, T* __restrict__ db, int B, int H, int d, int taps,
-                       const GradSlots slots) {
+                       const GradSlots slots, const FilterTerms terms) {
     __shared__ float part[kParts][128];
     tc::pdl_launch_dependents();
     tc::pdl_wait_primary();
@@ -289,12 +293,35 @@ grad_filter_sum_kernel(const float* __restrict__ sums, T* __restrict__ dw, T* __
             for (long long i = c0 + (slots.heads ? at : 0); i <= c1; i += slots.heads ? kParts : 1) s += slot(u + i);
         }
     }
-    part[at][c] = s;
-    __syncthreads();
-    if (at != 0 || c >= d) return;
-    float t = 0.f;
+    auto total = [&]() {
+        __syncthreads();
+        part[at][c] = s;
+        __syncthreads();
+        float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) t += part[i][c];
+        for (int i = 0; i < kParts; ++i) t += part[i][c];
+        return t;
+    };
+    float t = total();
+    const bool again = tap < taps && c < d && t != t;      // the same in all strands
+    if (__syncthreads_or(again)) {
+        s = 0.f;
+        const int dy = tap / terms.ksize - terms.ksize / 2, dx = tap % terms.ksize - terms.ksize / 2;
+        const int x0 = max(0, -dx), x1 = min(terms.gridW, terms.gridW - dx), y1 = min(terms.gridH, terms.gridH - dy);
+        for (int b = 0; again && b < B && s == s; ++b) {     // a NaN stays one
+            const long long plane = (long long)b * H + h;
+            const T* g = static_cast<const T*>(terms.g) + plane_offset(terms.lg, (int)plane, terms.hdiv) + c;
+            const T* v = static_cast<const T*>(terms.v) + plane_offset(terms.lv, (int)plane, terms.hdiv) + c;
+            for (int y = max(0, -dy) + at; y < y1 && s == s; y += kParts) {
+                const long long gt = terms.prefix + (long long)y * terms.gridW, vt = gt + (long long)dy * terms.gridW + dx;
+#pragma unroll 4
+                for (int x = x0; x < x1; ++x) s = fmaf(value(g + (gt + x) * terms.lg.token), value(v + (vt + x) * terms.lv.token), s);
+            }
+        }
+        const float by_terms = total();
+        if (again) t = by_terms;
+    }
+    if (at != 0 || c >= d) return;
     if (tap == taps) { if (db) put(db + h * d + c, t); }
     else if (dw) put(dw + ((size_t)h * d + c) * taps + tap, t);
 }
@@ -370,11 +397,12 @@ cudaError_t launch_grad_filters(const GradProblem& gp, const float* sums, const 
     const Problem& p = gp.p;
     const int taps = p.ksize * p.ksize;
     const dim3 grid((unsigned)(p.H * (taps + 1))), block((unsigned)((p.d + 31) / 32 * 32 * kParts));
+    const FilterTerms terms = {gp.g, p.v, gp.lg, p.lv, p.hdiv, p.prefix, p.gridH, p.gridW, p.ksize};
     // may set itself up while the kernel before it drains
     return p.bf16 ? tc::launch_programmatic(grad_filter_sum_kernel<__nv_bfloat16>, true, grid, block, 0, st, sums, static_cast<__nv_bfloat16*>(gp.dw),
-                                            static_cast<__nv_bfloat16*>(gp.db), p.B, p.H, p.d, taps, slots)
+                                            static_cast<__nv_bfloat16*>(gp.db), p.B, p.H, p.d, taps, slots, terms)
                   : tc::launch_programmatic(grad_filter_sum_kernel<float>, true, grid, block, 0, st, sums, static_cast<float*>(gp.dw), static_cast<float*>(gp.db),
-                                            p.B, p.H, p.d, taps, slots);
+                                            p.B, p.H, p.d, taps, slots, terms);
 }
 
 cudaError_t launch_filter_sums(const GradProblem& gp, float* sums, cudaStream_t st) {
