@@ -570,8 +570,9 @@ int castling_attn_backward(castling_attn_t* h, const void* q, const void* k, con
     if (tensor) {
         unsigned* status = p.status ? p.status : reinterpret_cast<unsigned*>(ws + castling::grad_workspace(p).status);
         e = castling::tc::grad(gp, ws, status, st, &launches, &h->timer);
-        if (e == cudaErrorNotSupported && !pinned) {   // strides that the tensor maps cannot take: the CUDA-core kernels take any layout
+        if (e == cudaErrorNotSupported) {   // strides that the tensor maps cannot take: the CUDA-core kernels take any layout
             (void)cudaGetLastError();
+            if (pinned) return CASTLING_ERR_UNSUPPORTED;
             tensor = false;
             h->timer.begin(st);
         }
