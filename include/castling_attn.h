@@ -354,12 +354,15 @@ typedef struct {
  *   another output; outputs may lie between one another as slices of one fused tensor do, with the same strides, others may not reach into one
  *   another.  The strides of an output nest: each is at least what the shorter ones reach.
  *
+ * The handle's first backward allocates its status word (256 bytes), during a capture too, and nothing else.  Under a max_workspace
+ * that has no room for it the kernels without waits are taken, on the CUDA cores (pinned to the tensor cores: OOM).
+ *
  * Sums over tokens, images and heads' filters are taken in fp32 in an order that depends on the shape alone: the same call
  * gives the same bits.  All tensors have one dtype, the filters' gradients too (rounded once from fp32 sums).  bf16 heads of width 64
  * and 32 with at least 48 tokens run on the tensor cores (filters of other sizes than 3x3 and 5x5: all but the gradient of v), everything
  * else on the CUDA cores.  A handle with normalize_rows,
  * exact_kernel or sparse_branch: UNSUPPORTED.  The current device has to be the handle's.  Errors: INVALID_ARG, UNSUPPORTED,
- * ALIGNMENT, CUDA.
+ * ALIGNMENT, CUDA, OOM.
  */
 CASTLING_API size_t castling_attn_backward_workspace_bytes(const castling_attn_t* handle, int B, int H, int gridH, int gridW, int d,
                           castling_dtype_t dtype);

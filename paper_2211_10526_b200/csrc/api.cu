@@ -15,6 +15,7 @@ struct castling_attn {
     int device = 0;
     float* ws = nullptr;        // header | state | partial
     size_t ws_bytes = 0;
+    unsigned* own_status = nullptr;  // of calls that need no workspace of the handle: never moved, captured graphs hold its address
     unsigned* counters = nullptr;  // arrival counters of the split reduction, zero between calls
     size_t counters_cap = 0;
     unsigned* more_counters = nullptr;  // an allocation of their own, where those behind the workspace became too few
@@ -141,18 +142,25 @@ int ensure_workspace(castling_attn* h, int BH, int N, int d, bool bf16) {
     return CASTLING_OK;
 }
 
-// A status word for a call that needs no workspace.  A call without one is not refused: during a capture, or under a cap that
-// leaves no room, it takes the kernels that do not wait.
-unsigned* status_word(castling_attn* h, cudaStream_t stream) {
-    if (!h->ws) {
-        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-        if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone ||
-            ensure_workspace(h, 1, 1, 16, false) != CASTLING_OK) {
-            (void)cudaGetLastError();
-            return nullptr;
-        }
-    }
-    return reinterpret_cast<unsigned*>(h->ws);
+// A status word for a call that needs no workspace.  The handle's first such call allocates it, during a capture too (nothing of that
+// is captured: a stream of its own clears it), so that which kernels a call takes does not depend on the calls before it.  A call without
+// one is not refused: under a cap that leaves no room, it takes the kernels that do not wait.
+unsigned* status_word(castling_attn* h) {
+    const size_t bytes = castling::kHeaderWords * sizeof(float);
+    if (h->own_status || (h->cfg.max_workspace && bytes > h->cfg.max_workspace)) return h->own_status;
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) { (void)cudaGetLastError(); return nullptr; }
+    unsigned* word = nullptr;
+    cudaStream_t st = nullptr;
+    cudaError_t e = cudaMalloc((void**)&word, bytes);
+    if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+    if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, bytes, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (st) cudaStreamDestroy(st);
+    if (e != cudaSuccess && word) cudaFree(word);
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return nullptr; }
+    return h->own_status = word;
 }
 
 }  // namespace
@@ -191,6 +199,7 @@ int castling_attn_create(const castling_attn_config_t* cfg, castling_attn_t** ou
 int castling_attn_destroy(castling_attn_t* h) {
     if (!h) return CASTLING_OK;
     if (h->ws) cudaFree(h->ws);
+    if (h->own_status) cudaFree(h->own_status);
     if (h->more_counters) cudaFree(h->more_counters);
     if (h->stage) cudaFree(h->stage);
     if (h->copy_in) cudaStreamDestroy(h->copy_in);
@@ -563,13 +572,16 @@ int castling_attn_backward(castling_attn_t* h, const void* q, const void* k, con
     const bool tensor_ok = castling::tc::grad_supports(p), pinned = h->cfg.force_path == CASTLING_PATH_TENSOR;
     if (pinned && !tensor_ok) return CASTLING_ERR_UNSUPPORTED;
     bool tensor = pinned || (h->cfg.force_path == CASTLING_PATH_AUTO && castling::tc::grad_preferred(p));
-    p.status = status_word(h, st);
+    p.status = status_word(h);
+    if (!p.status) {   // under a cap: kernels that do not wait
+        if (pinned) return CASTLING_ERR_OOM;
+        tensor = false;
+    }
     float* ws = static_cast<float*>(workspace);
     int launches = 0;
     h->timer.begin(st);
     if (tensor) {
-        unsigned* status = p.status ? p.status : reinterpret_cast<unsigned*>(ws + castling::grad_workspace(p).status);
-        e = castling::tc::grad(gp, ws, status, st, &launches, &h->timer);
+        e = castling::tc::grad(gp, ws, p.status, st, &launches, &h->timer);
         if (e == cudaErrorNotSupported) {   // strides that the tensor maps cannot take: the CUDA-core kernels take any layout
             (void)cudaGetLastError();
             if (pinned) return CASTLING_ERR_UNSUPPORTED;
@@ -587,17 +599,21 @@ int castling_attn_backward(castling_attn_t* h, const void* q, const void* k, con
 int castling_attn_device_status(castling_attn_t* h, void* stream, unsigned int* raw) {
     if (!h) return CASTLING_ERR_INVALID_ARG;
     unsigned int word = 0;
-    if (h->ws) {
+    for (const void* at : {static_cast<const void*>(h->ws), static_cast<const void*>(h->own_status)}) {
+        if (!at) continue;
+        unsigned int one = 0;
         cudaStream_t st = static_cast<cudaStream_t>(stream);
-        cudaError_t e = cudaMemcpyAsync(&word, h->ws, sizeof(word), cudaMemcpyDeviceToHost, st);
+        cudaError_t e = cudaMemcpyAsync(&one, at, sizeof(one), cudaMemcpyDeviceToHost, st);
         if (e != cudaSuccess) return fail_cuda(h, e);
         if ((e = cudaStreamSynchronize(st)) != cudaSuccess) return fail_cuda(h, e);
+        word |= one;
     }
     if (raw) *raw = word;
     if (word) {
         // reported once: the word is cleared, and so are arrival counters that a kernel which gave up may have
         // left half way
-        cudaMemset(h->ws, 0, sizeof(unsigned));
+        if (h->ws) cudaMemset(h->ws, 0, sizeof(unsigned));
+        if (h->own_status) cudaMemset(h->own_status, 0, sizeof(unsigned));
         if (h->counters) cudaMemset(h->counters, 0, h->counters_cap * sizeof(unsigned));
     }
     return word ? CASTLING_ERR_DEVICE : CASTLING_OK;
@@ -675,7 +691,7 @@ int castling_attn_shard_apply(castling_attn_t* h, const void* q, const void* v_h
         if (e == cudaErrorNotSupported) { (void)cudaGetLastError(); tensor = false; h->timer.begin(static_cast<cudaStream_t>(stream)); }
     }
     if (!tensor) {
-        if (!p.bf16) p.status = status_word(h, static_cast<cudaStream_t>(stream));
+        if (!p.bf16) p.status = status_word(h);
         e = castling::simt_forward(p, const_cast<float*>(state), nullptr, 1, static_cast<cudaStream_t>(stream), &launches,
                                    &h->timer);
     }

@@ -19,7 +19,6 @@ struct GradWorkspace {
     size_t S, T;               // states of k and v, of q and g, [BH] each
     size_t partial;            // token splits of one of them
     size_t counters;           // arrival counters of the tensor-core states' splits
-    size_t status;             // a status word for a call whose handle has none yet (nobody reads it)
     size_t filters;            // the filters turned around, in the tensors' type
     size_t sums;               // sums of the filters' gradients, [slots][taps + 1][d]
     size_t words;

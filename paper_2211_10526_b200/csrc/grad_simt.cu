@@ -425,7 +425,6 @@ GradWorkspace grad_workspace(const Problem& p) {
     w.T = at; at += up(p.BH * words);
     w.partial = at; at += up(P > 1 ? (size_t)p.BH * P * words : 0);
     w.counters = at; at += up((size_t)p.BH * tc::kCountersPerHead);
-    w.status = at; at += up(1);
     w.filters = at; at += up((size_t)p.H * p.d * taps);
     size_t slots = (size_t)p.BH * filter_slots(p);
     if (tc::grad_fused_supports(p) && (size_t)(p.H + tc::grad_fused_ctas(p)) > slots) slots = (size_t)(p.H + tc::grad_fused_ctas(p));
