@@ -102,7 +102,7 @@ class CastlingAttn:
 
     def backward(self, grad_out, q, k, v, dw_weight, gridH: int, gridW: int, bias: bool = True,
                  out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None) -> Tuple[Optional[torch.Tensor], ...]:
-        """Gradients of ``forward``: (grad_q, grad_k, grad_v, grad_dw_weight, grad_dw_bias) for the gradient of its output; q, k, v and
+        """Gradients of ``forward``, which keeps no history for autograd: (grad_q, grad_k, grad_v, grad_dw_weight, grad_dw_bias) for the gradient of its output; q, k, v and
         dw_weight are what the forward was given.  ``bias=False``: there was none, and the last gradient is None.  ``out``: tensors
         for the first three, e.g. slices of one ``[B, N, 3, H, d]`` gradient of a fused projection, without elements in common.  New tensors and a workspace
         come from torch's allocator, so that calls on several streams, and captured ones, do not share any.  A handle with a variant of

@@ -1,5 +1,6 @@
 """The operators around the attention core in a block of a network, on torch tensors: rotary positions on q and k, and the norms of
-the residual stream with its gates and scales.  Each has its gradients as a method of its own, like ``CastlingAttn.backward``; all
+the residual stream with its gates and scales.  Each has its gradients as a method of its own, like ``CastlingAttn.backward``: results have no
+autograd history, whether or not the inputs require gradients, and a training step chains the methods by hand.  All
 arithmetic is in the CUDA library.  Objects hold sizes and constants only: one serves any number of streams and threads.
 
 A block as a user writes it (``norm`` of the block before gave ``y``):
@@ -41,7 +42,7 @@ class GridRope:
 
     def forward(self, q, k: Optional[torch.Tensor] = None, grid: Optional[Tuple[int, ...]] = None, prefix_tokens: int = 0,
                 positions: Optional[torch.Tensor] = None, inplace: bool = False) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
-        """q ``[B, H, N, d]`` and k (its number of heads may be another; or None), any strides with stride 1 in the last dimension,
+        """q ``[B, H, N, d]`` and k (its number of heads may be another; or None), any strides but nought, 1 in the last dimension,
         float32 or bfloat16.  Either ``grid``, a size per axis, last axis fastest: the positions of the token grid behind
         ``prefix_tokens`` leading tokens, which are copied; or ``positions``, int32, int64 or float32, ``[B, N, axes]``, ``[1, N, axes]``
         or ``[N, axes]``, contiguous: a decoded token's, say.  Returns new (q, k), or with ``inplace`` the same ones, turned, which
@@ -95,7 +96,7 @@ class BlockNorm:
     def forward(self, x, branch: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
                 post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                 gate: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
-        """x and branch ``[B, N, D]`` (or ``[N, D]``: one sequence), any strides with stride 1 in the last dimension, float32 or bfloat16; parameters
+        """x and branch ``[B, N, D]`` (or ``[N, D]``: one sequence), any strides but nought, 1 in the last dimension, float32 or bfloat16; parameters
         ``[D]``, the gate ``[B, D]``, contiguous, of the same dtype.  Returns new contiguous (h, y); y is None without ``kind``, and h is x itself
         where there is no branch and residual_scale is 1."""
         r = _call.norm_forward(*self._head, x, branch, weight, bias, post_weight, post_bias, scale, gate)

@@ -5,8 +5,8 @@
 //   dv and the sums for the filters (tc_grad_values.cu: width 64, 3x3 filters), or the filters turned around, an apply pass with k and G in the
 //   place of q and V, and the sums for the filters on their own,
 //   rows of q and k (tc_grad_rows.cu), addition of the sums.
-// Unit rows in the states are pairs of bf16 (FINE in tc_state.cu), as are the states behind them: results differ from the
-// definition by the rounding of outputs.
+// Unit rows in the states are pairs of bf16 (FINE in tc_state.cu), as are the states behind them in every product; rows of q and k meet them as they
+// came, with 1 / |x| in fp32.  Results differ from the definition by the rounding of outputs and about 2^-17 of the terms.
 #include "grad.cuh"
 #include "state_splits.cuh"
 #include "tc_host.cuh"
