@@ -84,11 +84,17 @@ bool encode_tensor_map(CUtensorMap* out, const void* base, const Shape& s) {
         estride[i] = 1;
         if (i + 1 < s.rank) gstride[i] = s.strides[i] * s.bytes;
     }
-    const CUresult r = g_encode(out, s.bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (cuuint32_t)s.rank, const_cast<void*>(base), gdim,
-                                gstride, bdim, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                s.swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : s.swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
-                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS;
+    auto encode = [&]() {
+        return g_encode(out, s.bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (cuuint32_t)s.rank, const_cast<void*>(base), gdim,
+                        gstride, bdim, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        s.swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : s.swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    if (encode()) return true;
+    // The driver's call wants a current context, which a thread has from its first launch or allocation on only: without this a thread that
+    // begins with a call of this library took the CUDA-core kernels.
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode();
 }
 }  // namespace
 
