@@ -15,7 +15,7 @@ struct castling_attn {
     int device = 0;
     float* ws = nullptr;        // header | state | partial
     size_t ws_bytes = 0;
-    unsigned* own_status = nullptr;  // of calls that need no workspace of the handle: never moved, captured graphs hold its address
+    std::atomic<unsigned*> own_status{nullptr};  // of calls that need no workspace of the handle: never moved, captured graphs hold its address
     unsigned* counters = nullptr;  // arrival counters of the split reduction, zero between calls
     size_t counters_cap = 0;
     unsigned* more_counters = nullptr;  // an allocation of their own, where those behind the workspace became too few
@@ -144,10 +144,11 @@ int ensure_workspace(castling_attn* h, int BH, int N, int d, bool bf16) {
 
 // A status word for a call that needs no workspace.  The handle's first such call allocates it, during a capture too (nothing of that
 // is captured: a stream of its own clears it), so that which kernels a call takes does not depend on the calls before it.  A call without
-// one is not refused: under a cap that leaves no room, it takes the kernels that do not wait.
+// one is not refused: under a cap that leaves no room, it takes the kernels that do not wait.  Of first calls at the same time, one's word is kept.
 unsigned* status_word(castling_attn* h) {
     const size_t bytes = castling::kHeaderWords * sizeof(float);
-    if (h->own_status || (h->cfg.max_workspace && bytes > h->cfg.max_workspace)) return h->own_status;
+    unsigned* have = h->own_status.load(std::memory_order_acquire);
+    if (have || (h->cfg.max_workspace && bytes > h->cfg.max_workspace)) return have;
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
     if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) { (void)cudaGetLastError(); return nullptr; }
     unsigned* word = nullptr;
@@ -157,10 +158,11 @@ unsigned* status_word(castling_attn* h) {
     if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, bytes, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (st) cudaStreamDestroy(st);
+    if (e == cudaSuccess && !h->own_status.compare_exchange_strong(have, word, std::memory_order_acq_rel)) e = cudaErrorNotReady;   // `have` is the other's
     if (e != cudaSuccess && word) cudaFree(word);
     (void)cudaThreadExchangeStreamCaptureMode(&mode);
-    if (e != cudaSuccess) { (void)cudaGetLastError(); return nullptr; }
-    return h->own_status = word;
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return have; }
+    return word;
 }
 
 }  // namespace
@@ -199,7 +201,7 @@ int castling_attn_create(const castling_attn_config_t* cfg, castling_attn_t** ou
 int castling_attn_destroy(castling_attn_t* h) {
     if (!h) return CASTLING_OK;
     if (h->ws) cudaFree(h->ws);
-    if (h->own_status) cudaFree(h->own_status);
+    if (unsigned* word = h->own_status.load()) cudaFree(word);
     if (h->more_counters) cudaFree(h->more_counters);
     if (h->stage) cudaFree(h->stage);
     if (h->copy_in) cudaStreamDestroy(h->copy_in);
@@ -599,7 +601,8 @@ int castling_attn_backward(castling_attn_t* h, const void* q, const void* k, con
 int castling_attn_device_status(castling_attn_t* h, void* stream, unsigned int* raw) {
     if (!h) return CASTLING_ERR_INVALID_ARG;
     unsigned int word = 0;
-    for (const void* at : {static_cast<const void*>(h->ws), static_cast<const void*>(h->own_status)}) {
+    unsigned* const own = h->own_status.load(std::memory_order_acquire);
+    for (const void* at : {static_cast<const void*>(h->ws), static_cast<const void*>(own)}) {
         if (!at) continue;
         unsigned int one = 0;
         cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -613,7 +616,7 @@ int castling_attn_device_status(castling_attn_t* h, void* stream, unsigned int* 
         // reported once: the word is cleared, and so are arrival counters that a kernel which gave up may have
         // left half way
         if (h->ws) cudaMemset(h->ws, 0, sizeof(unsigned));
-        if (h->own_status) cudaMemset(h->own_status, 0, sizeof(unsigned));
+        if (own) cudaMemset(own, 0, sizeof(unsigned));
         if (h->counters) cudaMemset(h->counters, 0, h->counters_cap * sizeof(unsigned));
     }
     return word ? CASTLING_ERR_DEVICE : CASTLING_OK;

@@ -108,3 +108,31 @@ def test_under_a_cap_without_room():
         with pytest.raises(b.CastlingError) as error:
             attn.backward(*t, 14, 14)
         assert error.value.code == b.ERR_OOM
+
+
+def test_first_calls_at_the_same_time():
+    import threading
+    from paper_2211_10526_b200 import CastlingAttn
+    for shape, dtype in (((2, 3, 14, 14, 64, 3), BF16), ((1, 2, 30, 20, 64, 5), BF16), ((2, 3, 20, 20, 64, 3), F32)):
+        t = tensors(shape, dtype, 7)
+        with CastlingAttn(ksize=shape[5]) as attn:
+            want = attn.backward(*t, shape[2], shape[3])
+        torch.cuda.synchronize()
+        for _ in range(5):
+            with CastlingAttn(ksize=shape[5]) as attn:
+                got, start = [None] * 6, threading.Barrier(6)
+
+                def call(i):
+                    with torch.cuda.stream(torch.cuda.Stream()):
+                        start.wait()
+                        got[i] = attn.backward(*t, shape[2], shape[3])
+                        torch.cuda.current_stream().synchronize()
+
+                threads = [threading.Thread(target=call, args=(i,)) for i in range(6)]
+                for x in threads:
+                    x.start()
+                for x in threads:
+                    x.join()
+                torch.cuda.synchronize()
+                assert all(g is not None and same(g, want) for g in got)
+                assert attn.device_status() == (0, 0)
